@@ -493,14 +493,19 @@ def _vector(t: Optional[torch.Tensor], n: int, dtype: torch.dtype, what: str) ->
 
 
 def _scratch(nbytes: int, given: Optional[torch.Tensor], device: torch.device, stream):
-    """(tensor, pointer, size) of a call's workspace: the caller's, or one made here, which the allocator may
-    hand out again once `stream` has passed the call."""
+    """(tensor, pointer, size) of a call's workspace: the caller's, or one made here.  The latter is allocated under the
+    call's stream: the allocator's blocks belong to streams, and one of the current stream's may have users still
+    queued there that nothing orders before a call on another."""
     if nbytes == 0:
         return None, None, 0
     if given is None:
-        given = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        if stream is not None:
-            given.record_stream(stream if isinstance(stream, torch.Stream) else torch.cuda.ExternalStream(int(stream), device=device))
+        if stream is None:
+            given = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        else:
+            if not isinstance(stream, torch.Stream):
+                stream = torch.cuda.ExternalStream(_operator_stream(stream, device), device=device)
+            with torch.cuda.stream(stream):
+                given = torch.empty(nbytes, dtype=torch.uint8, device=device)
     elif not given.is_cuda or given.dtype != torch.uint8 or not given.is_contiguous():
         raise ValueError("workspace must be a contiguous uint8 device tensor")
     return given, given.data_ptr(), given.numel()
