@@ -460,7 +460,7 @@ class Mxfp:
         if tensor.dtype != torch.uint8 or not tensor.is_contiguous() or tensor.numel() < nbytes:
             raise ValueError("a container is a contiguous uint8 tensor of sbc_mxfp_bytes(rows, cols) bytes")
         self.rows, self.cols, self.tensor = rows, cols, tensor
-        self.ptr = tensor.data_ptr()
+        self.ptr, self.device = tensor.data_ptr(), tensor.get_device()
 
 
 # (the sizes below follow from their arguments alone, and a call through ctypes takes a microsecond)
@@ -469,10 +469,16 @@ def sbc_mxfp_bytes(rows: int, cols: int) -> int:
     return load().sbc_mxfp_bytes(rows, cols)
 
 
-def _dense(t: torch.Tensor, what: str):
-    """(pointer, type, rows, columns, leading dimension) of a matrix whose columns lie side by side."""
-    if not t.is_cuda:
-        raise ValueError("libsbc works on device memory: expected a CUDA/HIP tensor")
+def _same_device(on: int, device: int, what: str) -> None:
+    if on != device:
+        raise ValueError("%s must lie on the device of the call's first matrix" % what)
+
+
+def _dense(t: torch.Tensor, what: str, device: Optional[int] = None):
+    """(pointer, type, rows, columns, leading dimension) of a matrix whose columns lie side by side; on `device` if given."""
+    _check_device(t)
+    if device is not None:
+        _same_device(t.get_device(), device, what)
     kind = SBC_TYPES.get(t.dtype)
     if kind is None or t.dim() != 2:
         raise ValueError("%s must be a matrix of float32, bfloat16 or float16" % what)
@@ -483,12 +489,18 @@ def _dense(t: torch.Tensor, what: str):
     return t.data_ptr(), kind, rows, cols, ld if rows > 1 else max(cols, 1)
 
 
-def _vector(t: Optional[torch.Tensor], n: int, dtype: torch.dtype, what: str) -> Optional[int]:
-    """Pointer of a contiguous device tensor of n values (None for None)."""
+def _held(q: "Mxfp", device: int, what: str) -> int:
+    """Pointer of a container."""
+    _same_device(q.device, device, what)
+    return q.ptr
+
+
+def _vector(t: Optional[torch.Tensor], n: int, dtype: torch.dtype, device: int, what: str) -> Optional[int]:
+    """Pointer of a contiguous tensor of n values on the call's device (None for None)."""
     if t is None:
         return None
-    if not t.is_cuda or t.dtype != dtype or t.numel() != n or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous device tensor of %d values of %s" % (what, n, dtype))
+    if t.get_device() != device or t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous tensor of %d values of %s on the call's device" % (what, n, dtype))
     return t.data_ptr()
 
 
@@ -506,8 +518,8 @@ def _scratch(nbytes: int, given: Optional[torch.Tensor], device: torch.device, s
                 stream = torch.cuda.ExternalStream(_operator_stream(stream, device), device=device)
             with torch.cuda.stream(stream):
                 given = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    elif not given.is_cuda or given.dtype != torch.uint8 or not given.is_contiguous():
-        raise ValueError("workspace must be a contiguous uint8 device tensor")
+    elif given.device != device or given.dtype != torch.uint8 or not given.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor on the call's device")
     return given, given.data_ptr(), given.numel()
 
 
@@ -517,7 +529,11 @@ def _operator_stream(stream, device: torch.device):
         if _raw_stream is not None:
             return _raw_stream(device.index)
         stream = torch.cuda.current_stream(device)
-    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+    if not hasattr(stream, "cuda_stream"):
+        return int(stream)
+    if getattr(stream, "device", device) != device:
+        raise ValueError("stream must belong to the call's device")
+    return stream.cuda_stream
 
 
 def _checked(rc: int, where: str) -> None:
@@ -534,8 +550,8 @@ def sbc_mxfp_quantize(x: torch.Tensor, by_rows: Optional[Mxfp] = None, by_cols: 
     if by_cols is not None and (by_cols.rows, by_cols.cols) != (cols, rows):
         raise ValueError("by_cols must be a container of the transposed shape")
     _checked(load().sbc_mxfp_quantize(x.device.index, _operator_stream(stream, x.device), ptr, kind, rows, cols, ld,
-                                      by_rows.ptr if by_rows is not None else None,
-                                      by_cols.ptr if by_cols is not None else None), "sbc_mxfp_quantize")
+                                      _held(by_rows, x.device.index, "by_rows") if by_rows is not None else None,
+                                      _held(by_cols, x.device.index, "by_cols") if by_cols is not None else None), "sbc_mxfp_quantize")
 
 
 def sbc_mxfp_dequantize(q: Mxfp, out: torch.Tensor, stream=None) -> None:
@@ -543,7 +559,7 @@ def sbc_mxfp_dequantize(q: Mxfp, out: torch.Tensor, stream=None) -> None:
     ptr, kind, rows, cols, ld = _dense(out, "out")
     if (q.rows, q.cols) != (rows, cols):
         raise ValueError("out must have the container's shape")
-    _checked(load().sbc_mxfp_dequantize(out.device.index, _operator_stream(stream, out.device), q.ptr, rows, cols, ptr, kind, ld),
+    _checked(load().sbc_mxfp_dequantize(out.device.index, _operator_stream(stream, out.device), _held(q, out.device.index, "q"), rows, cols, ptr, kind, ld),
              "sbc_mxfp_dequantize")
 
 
@@ -552,7 +568,8 @@ def sbc_mxfp_matmul(a: Mxfp, b: Mxfp, out: torch.Tensor, stream=None) -> None:
     ptr, kind, m, n, ld = _dense(out, "out")
     if a.cols != b.cols or (a.rows, b.rows) != (m, n):
         raise ValueError("out must be a.rows x b.rows, and a and b have as many columns")
-    _checked(load().sbc_mxfp_matmul(out.device.index, _operator_stream(stream, out.device), a.ptr, b.ptr, m, n, a.cols, ptr, kind, ld),
+    device = out.device.index
+    _checked(load().sbc_mxfp_matmul(device, _operator_stream(stream, out.device), _held(a, device, "a"), _held(b, device, "b"), m, n, a.cols, ptr, kind, ld),
              "sbc_mxfp_matmul")
 
 
@@ -564,12 +581,13 @@ def sbc_mxfp_linear_workspace(m: int, k: int) -> int:
 def sbc_mxfp_linear(x: torch.Tensor, w: Mxfp, out: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """out[M, N] = Q(x) w^T for x[M, K], rounded to 4 bits within the call, and a container w of N x K; one token or many."""
     xp, kind, m, k, ldx = _dense(x, "x")
-    yp, out_kind, rows, n, ldy = _dense(out, "out")
+    device = x.device.index
+    yp, out_kind, rows, n, ldy = _dense(out, "out", device)
     if w.cols != k or w.rows != n or rows != m or kind != out_kind:
         raise ValueError("x must be M x w.cols and out M x w.rows of the same type")
     lib = load()
     keep, wp, wn = _scratch(sbc_mxfp_linear_workspace(m, k), workspace, x.device, stream)
-    _checked(lib.sbc_mxfp_linear(x.device.index, _operator_stream(stream, x.device), xp, kind, ldx, m, w.ptr, n, k, yp, ldy, wp, wn),
+    _checked(lib.sbc_mxfp_linear(device, _operator_stream(stream, x.device), xp, kind, ldx, m, _held(w, device, "w"), n, k, yp, ldy, wp, wn),
              "sbc_mxfp_linear")
 
 
@@ -588,9 +606,10 @@ def sbc_top_logits(logits: torch.Tensor, index: torch.Tensor, top: torch.Tensor,
     k = index.shape[1]
     lib = load()
     keep, wp, wn = _scratch(sbc_top_logits_workspace(rows, vocab, k), workspace, logits.device, stream)
-    _checked(lib.sbc_top_logits(logits.device.index, _operator_stream(stream, logits.device), ptr, kind, ld, rows, vocab, k, temperature,
-                                _vector(index, rows * k, torch.int32, "index"), _vector(top, rows * k, torch.float32, "top"),
-                                _vector(lse, rows, torch.float32, "lse"), wp, wn), "sbc_top_logits")
+    device = logits.device.index
+    _checked(lib.sbc_top_logits(device, _operator_stream(stream, logits.device), ptr, kind, ld, rows, vocab, k, temperature,
+                                _vector(index, rows * k, torch.int32, device, "index"), _vector(top, rows * k, torch.float32, device, "top"),
+                                _vector(lse, rows, torch.float32, device, "lse"), wp, wn), "sbc_top_logits")
 
 
 @functools.lru_cache(maxsize=4096)
@@ -599,7 +618,7 @@ def sbc_distill_workspace(rows: int, vocab: int) -> int:
 
 
 def _like(t: torch.Tensor, logits: torch.Tensor, what: str):
-    ptr, _, _, _, ld = _dense(t, what)
+    ptr, _, _, _, ld = _dense(t, what, logits.get_device())
     if t.dtype != logits.dtype or t.shape != logits.shape:
         raise ValueError("%s must have the shape and type of logits" % what)
     return ptr, ld
@@ -618,11 +637,12 @@ def sbc_distill_loss(logits: torch.Tensor, index: torch.Tensor, top: torch.Tenso
     gp, ldg = _like(grad, logits, "grad") if grad is not None else (None, 0)
     lib = load()
     keep, wp, wn = _scratch(sbc_distill_workspace(rows, vocab), workspace, logits.device, stream)
-    _checked(lib.sbc_distill_loss(logits.device.index, _operator_stream(stream, logits.device), ptr, kind, ld, rows, vocab,
-                                  _vector(index, rows * k, torch.int32, "index"), _vector(top, rows * k, torch.float32, "top"), k,
-                                  _vector(teacher_lse, rows, torch.float32, "teacher_lse"), temperature,
-                                  _vector(weight, rows, torch.float32, "weight"), _vector(loss, rows, torch.float32, "loss"),
-                                  _vector(stats, rows * 4, torch.float32, "stats"), gp, ldg, wp, wn), "sbc_distill_loss")
+    device = logits.device.index
+    _checked(lib.sbc_distill_loss(device, _operator_stream(stream, logits.device), ptr, kind, ld, rows, vocab,
+                                  _vector(index, rows * k, torch.int32, device, "index"), _vector(top, rows * k, torch.float32, device, "top"), k,
+                                  _vector(teacher_lse, rows, torch.float32, device, "teacher_lse"), temperature,
+                                  _vector(weight, rows, torch.float32, device, "weight"), _vector(loss, rows, torch.float32, device, "loss"),
+                                  _vector(stats, rows * 4, torch.float32, device, "stats"), gp, ldg, wp, wn), "sbc_distill_loss")
 
 
 def sbc_distill_grad(logits: torch.Tensor, index: torch.Tensor, top: torch.Tensor, temperature: float, stats: torch.Tensor,
@@ -634,8 +654,9 @@ def sbc_distill_grad(logits: torch.Tensor, index: torch.Tensor, top: torch.Tenso
         raise ValueError("index must be rows x k")
     k = index.shape[1]
     gp, ldg = _like(grad, logits, "grad")
-    _checked(load().sbc_distill_grad(logits.device.index, _operator_stream(stream, logits.device), ptr, kind, ld, rows, vocab,
-                                     _vector(index, rows * k, torch.int32, "index"), _vector(top, rows * k, torch.float32, "top"), k,
-                                     _vector(teacher_lse, rows, torch.float32, "teacher_lse"), temperature,
-                                     _vector(stats, rows * 4, torch.float32, "stats"), _vector(dloss, rows, torch.float32, "dloss"), gp, ldg),
+    device = logits.device.index
+    _checked(load().sbc_distill_grad(device, _operator_stream(stream, logits.device), ptr, kind, ld, rows, vocab,
+                                     _vector(index, rows * k, torch.int32, device, "index"), _vector(top, rows * k, torch.float32, device, "top"), k,
+                                     _vector(teacher_lse, rows, torch.float32, device, "teacher_lse"), temperature,
+                                     _vector(stats, rows * 4, torch.float32, device, "stats"), _vector(dloss, rows, torch.float32, device, "dloss"), gp, ldg),
              "sbc_distill_grad")
