@@ -765,7 +765,8 @@ __device__ __forceinline__ float distill_row(const ListSums& l, ExpSum rest, con
     const bool odd = threadIdx.x & 1u;
     const float m = fmaxf(rest.base, l.peak), top = finite_base(m);
     const bool empty = rest.base == -__builtin_inff() && rest.sum == 0.0f;
-    const double below = ((double)finite_base(l.peak) - (double)top) * a.inv_t, rest_below = ((double)rest.base - (double)top) * a.inv_t;
+    // (a list of nothing but -inf has no part in the sum: its exponential, of how far 0 lies above the others, may be infinite)
+    const double below = l.peak == -__builtin_inff() ? 0.0 : ((double)l.peak - (double)top) * a.inv_t, rest_below = ((double)rest.base - (double)top) * a.inv_t;
     const double downs = exp(odd ? rest_below : below), down = empty ? 0.0 : lane_of(downs, 1);
     const double listed = l.listed * lane_of(downs, 0), r = rest.sum * down, sum = listed + r;
     const double logs = log(odd ? (double)rest.sum : sum), log_z = lane_of(logs, 0);
@@ -798,7 +799,7 @@ __device__ __forceinline__ float distill_row(const ListSums& l, ExpSum rest, con
 // Gradient of the listed entries.
 template <typename T>
 __device__ __forceinline__ void store_list(const ListSums& l, const Slots& z, T* g, const DistillStats& st, float factor, const DistillArgs& a) {
-    const double share = st.share * exp(((double)finite_base(l.peak) - (double)st.top) * a.inv_t);
+    const double share = st.share * (l.peak == -__builtin_inff() ? 0.0 : exp(((double)l.peak - (double)st.top) * a.inv_t));
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         if (l.first[i]) g[z.index[i]] = (T)(float)(factor * (share * l.e[i] - l.sum[i]));
