@@ -398,7 +398,7 @@ int sbc_top_logits(int device, void* hip_stream, const void* logits, int type, i
                    double temperature, int32_t* index, float* top, float* lse, void* workspace, size_t workspace_bytes);
 
 /* Loss of a student against a teacher's top logits.  With s = logits / T, q = softmax(s) and the teacher's slots
- * (index, top) of the row, of which those count whose index lies in [0, vocab) and whose logit is above -inf:
+ * (index, top) of the row, of which those count whose index lies in [0, vocab) and whose logit is above -inf (NaN is not):
  *     p_j   = softmax of top / T over the slots that count               without teacher_lse, or
  *     p_j   = exp(top_j / T - teacher_lse), p_rest = max(0, 1 - sum p_j)   with it: the teacher's other words as a class
  *     loss  = T^2 (sum p_j (log p_j - log q_j) + p_rest (log p_rest - log q_rest))

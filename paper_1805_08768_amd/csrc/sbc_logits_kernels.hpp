@@ -641,6 +641,9 @@ struct Slots {
 };
 constexpr uint32_t kNoSlot = 0xffffffffu;
 
+// (a logit of NaN is not above -inf)
+__device__ __forceinline__ bool slot_counts(uint32_t index, float t, uint32_t vocab) { return index < vocab && t > -__builtin_inff(); }
+
 template <typename T> __device__ __forceinline__ void slots_fetch(Slots& z, const DistillArgs& a, int64_t row, uint32_t vocab, const T* x) {
     const uint32_t lane = threadIdx.x & 63u;
 #pragma unroll
@@ -655,7 +658,7 @@ template <typename T> __device__ __forceinline__ void slots_fetch(Slots& z, cons
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if (z.index[i] >= vocab || z.t[i] == -__builtin_inff()) z.index[i] = kNoSlot;
+        if (!slot_counts(z.index[i], z.t[i], vocab)) z.index[i] = kNoSlot;
         z.s[i] = z.index[i] != kNoSlot ? (float)x[z.index[i]] : -__builtin_inff();
     }
 }
@@ -1070,7 +1073,7 @@ __global__ __launch_bounds__(kPartThreads) void k_distill_part(const T* __restri
     __syncthreads();
     if (threadIdx.x < a.k) {
         const uint32_t index = (uint32_t)a.index[row * a.k + threadIdx.x], at = index + x.lead, vec = (at >> 3) - first;
-        if (index < vocab && vec < vecs && !(a.top[row * a.k + threadIdx.x] == -__builtin_inff())) atomicOr(&marks[vec >> 2], 1u << ((vec & 3u) * 8u + (at & 7u)));
+        if (slot_counts(index, a.top[row * a.k + threadIdx.x], vocab) && vec < vecs) atomicOr(&marks[vec >> 2], 1u << ((vec & 3u) * 8u + (at & 7u)));
     }
     __syncthreads();
     const ExpSum s = block_join(sum_unlisted<T, kPartThreads>(x, first, vecs, reinterpret_cast<const uint8_t*>(marks), a.c), sums, kPartThreads / 64, a.c);
