@@ -58,13 +58,28 @@ template <typename T> struct Row {
     }
 };
 
-// The largest of three; a NaN loses against a number.  (fmaxf has each operand quieted by an instruction of its own.)
+// The largest of three; a quiet NaN loses against a number, but a signalling one, as a type's bits may hold it, counts as a quiet
+// one before the third is looked at, so that a larger number beside it is lost.
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
     asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
     return d;
 }
 __device__ __forceinline__ float max8(const float (&v)[8]) { return max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), max3(v[6], v[7], v[7])); }
+
+// The same, where any NaN wins; and of numbers alone (-inf where there is none).
+__device__ __forceinline__ float maximum3(float a, float b, float c) {
+    float d;
+    asm("v_maximum3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+    return d;
+}
+__device__ __forceinline__ float maximum8(const float (&v)[8]) { return maximum3(maximum3(v[0], v[1], v[2]), maximum3(v[3], v[4], v[5]), maximum3(v[6], v[7], v[7])); }
+__device__ __forceinline__ float number8(const float (&v)[8]) {
+    float w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = v[j] == v[j] ? v[j] : -__builtin_inff();
+    return max8(w);
+}
 
 // Reductions over a wavefront, all of whose lanes take part: rows of 16 lanes by exchanges within the row, then the
 // four rows, the same order for every lane.
@@ -391,7 +406,7 @@ __device__ __forceinline__ uint32_t top_digest(TopShared<threads>& sh, const Row
             uint32_t order[n];
 #pragma unroll
             for (int i = 0; i < n; ++i) {
-                const float m = max8(v[i]);
+                const float m = max8(v[i]);         // (or less, beside a NaN: a floor all the same)
                 order[i] = m >= tau ? top_order(m) : 0u;
             }
             const uint32_t floor_ = block_least(sh.tally, turn, wave_floor(order, (k + kTopWaves - 1) / kTopWaves));
@@ -472,13 +487,21 @@ __global__ __launch_bounds__(threads) void k_top(const T* __restrict__ logits, i
     for (uint32_t from = first; from < end; from += n * threads) {
         float v[n][8], most[n];
         float m = s.base;
+        bool nan = false;
 #pragma unroll
         for (int i = 0; i < n; ++i) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[i][j] = (float)raw[i][j];
-            most[i] = max8(v[i]);
-            m = fmaxf(m, most[i]);
+            most[i] = maximum8(v[i]);
+            nan |= most[i] != most[i];
         }
+        // (a NaN must not hide the numbers beside it, and there hardly is one)
+        if (__any(nan)) {
+#pragma unroll
+            for (int i = 0; i < n; ++i) most[i] = number8(v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < n; ++i) m = fmaxf(m, most[i]);
         if (from + n * threads < end) load(from + n * threads);
         if (out.lse) {
             const float b = lse_base(m);
