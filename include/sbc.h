@@ -340,7 +340,9 @@ int sbc_copy_baseline(void* hip_stream, void* dst, const void* src, size_t bytes
  * graph.  Calls share nothing but the buffers they are given, which must stay as they are until the stream
  * has passed the call.  Matrices are dense, row by row, `ld` values from one row to the next
  * (ld >= columns), aligned to their type; every type is an sbc_type, and sums are formed in 32 bits or more.
- * Rows may be 0 (nothing is enqueued), other sizes lie in [1, 2^31).  Errors: SBC_EINVAL (null or misaligned
+ * Rows may be 0 (nothing is enqueued), other sizes lie in [1, 2^31).  What a call writes (outputs, the workspace it
+ * asked for) overlaps nothing else that it is given, but where its comment says so; matrices whose rows lie beside each other
+ * in one buffer, with the same ld, do not overlap.  Errors: SBC_EINVAL (null, misaligned or overlapping
  * pointers, sizes, types, no such device), SBC_ECAPACITY (a workspace below what its function asks for,
  * a matrix of more than 2^22 tiles of 128 x 128, a product of up to 16 rows with more than 2^26 columns), SBC_EHIP; nothing is enqueued after the first two. */
 typedef enum sbc_type { SBC_F32 = 0, SBC_BF16 = 1, SBC_F16 = 2 } sbc_type;

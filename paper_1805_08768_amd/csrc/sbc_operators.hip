@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 #include "sbc_mxfp_kernels.hpp"
 #include "sbc_logits_kernels.hpp"
@@ -40,6 +41,50 @@ bool dim_ok(int64_t n) { return n >= 1 && n < kMostDim; }
 // a dense matrix of `rows` rows, ld values apart
 bool dense_ok(const void* x, int type, int64_t cols, int64_t ld) { return x && size_of(type) && aligned(x, size_of(type)) && ld >= cols && ld < ((int64_t)1 << 40); }
 bool held_ok(const void* q) { return q && aligned(q, 16); }
+
+// The memory of an argument: `rows` runs of `run` bytes, `ld` bytes from one to the next.  None for a null pointer.
+struct Span {
+    uintptr_t from = 0, end = 0;
+    uint64_t rows = 0, run = 0, ld = 0;
+    Span(const void* p, uint64_t rows_, uint64_t run_, uint64_t ld_) {
+        if (!p || !rows_ || !run_) return;
+        from = reinterpret_cast<uintptr_t>(p);
+        rows = rows_;
+        run = run_;
+        ld = ld_;
+        uint64_t past;                                         // (beyond all addresses where the product is)
+        if (__builtin_mul_overflow(rows - 1, ld, &past) || __builtin_add_overflow(past, run, &past) || __builtin_add_overflow(past, from, &past)) past = UINT64_MAX;
+        end = past;
+    }
+    Span(const void* p, uint64_t bytes) : Span(p, 1, bytes, bytes) {}
+};
+Span matrix_span(const void* p, int type, int64_t rows, int64_t cols, int64_t ld) {
+    const uint64_t size = size_of(type);
+    return {p, (uint64_t)rows, (uint64_t)cols * size, (uint64_t)ld * size};
+}
+
+// Whether two arguments share no byte.  Rows the same distance apart may lie beside each other in one buffer; of other
+// matrices that lie among each other it is not said.
+bool apart(const Span& a, const Span& b) {
+    if (!a.rows || !b.rows || a.end <= b.from || b.end <= a.from) return true;
+    if (a.rows == 1 && b.rows == 1) return false;
+    const uint64_t ld = a.rows > 1 ? a.ld : b.ld;
+    if (b.rows > 1 && b.ld != ld) return false;
+    const uint64_t behind = b.from >= a.from ? (b.from - a.from) % ld : ld - 1 - (a.from - b.from - 1) % ld;      // of b's runs' starts behind a's
+    return a.run <= behind && behind + b.run <= ld;
+}
+
+// Whether what a call writes is apart from itself and from what it reads.
+bool apart(std::initializer_list<Span> written, std::initializer_list<Span> read) {
+    for (const Span* w = written.begin(); w != written.end(); ++w) {
+        for (const Span* other = written.begin(); other != w; ++other)
+            if (!apart(*w, *other)) return false;
+        for (const Span& r : read)
+            if (!apart(*w, r)) return false;
+    }
+    return true;
+}
+Span held_span(const void* q, int64_t rows, int64_t cols) { return {q, (uint64_t)(mx_panels(rows) * mx_steps(cols)) * (kMxPanelBytes + kMxScaleBytes)}; }
 
 MxPtr container(const void* q, int64_t rows, int64_t cols) {
     uint8_t* const p = static_cast<uint8_t*>(const_cast<void*>(q));
@@ -235,6 +280,7 @@ int sbc_mxfp_quantize(int device, void* hip_stream, const void* x, int type, int
     if (!dim_ok(rows) || !dim_ok(cols) || !dense_ok(x, type, cols, ld) || (!by_rows && !by_cols) || by_rows == by_cols) return SBC_EINVAL;
     if ((by_rows && !held_ok(by_rows)) || (by_cols && !held_ok(by_cols))) return SBC_EINVAL;
     if (!tiles_fit(rows, cols)) return SBC_ECAPACITY;
+    if (!apart({held_span(by_rows, rows, cols), held_span(by_cols, cols, rows)}, {matrix_span(x, type, rows, cols, ld)})) return SBC_EINVAL;
     if (const int rc = device_status(device)) return rc;
     DeviceScope scope(device);
     return by_type(type, [&](auto t) {
@@ -247,6 +293,7 @@ int sbc_mxfp_dequantize(int device, void* hip_stream, const void* q, int64_t row
     if (rows == 0 && dim_ok(cols) && size_of(type)) return SBC_OK;
     if (!dim_ok(rows) || !dim_ok(cols) || !held_ok(q) || !dense_ok(y, type, cols, ld)) return SBC_EINVAL;
     if (!tiles_fit(rows, cols)) return SBC_ECAPACITY;
+    if (!apart({matrix_span(y, type, rows, cols, ld)}, {held_span(q, rows, cols)})) return SBC_EINVAL;
     if (const int rc = device_status(device)) return rc;
     DeviceScope scope(device);
     return by_type(type, [&](auto t) {
@@ -262,6 +309,7 @@ int sbc_mxfp_matmul(int device, void* hip_stream, const void* a, const void* b, 
     if (M == 0 && dim_ok(N) && dim_ok(K) && size_of(type)) return SBC_OK;
     if (!dim_ok(M) || !dim_ok(N) || !dim_ok(K) || !held_ok(a) || !held_ok(b) || !dense_ok(c, type, N, ldc)) return SBC_EINVAL;
     if (!product_fits(M, N)) return SBC_ECAPACITY;
+    if (!apart({matrix_span(c, type, M, N, ldc)}, {held_span(a, M, K), held_span(b, N, K)})) return SBC_EINVAL;
     if (const int rc = device_status(device)) return rc;
     DeviceScope scope(device);
     return by_type(type, [&](auto t) {
@@ -280,6 +328,7 @@ int sbc_mxfp_linear(int device, void* hip_stream, const void* x, int type, int64
     const size_t room = sbc_mxfp_linear_workspace(M, K);
     if (room && !held_ok(workspace)) return SBC_EINVAL;
     if (workspace_bytes < room || !product_fits(M, N) || !tiles_fit(M, K)) return SBC_ECAPACITY;
+    if (!apart({matrix_span(y, type, M, N, ldy), {workspace, room}}, {matrix_span(x, type, M, K, ldx), held_span(w, N, K)})) return SBC_EINVAL;
     if (const int rc = device_status(device)) return rc;
     DeviceScope scope(device);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
@@ -309,6 +358,8 @@ int sbc_top_logits(int device, void* hip_stream, const void* logits, int type, i
     const size_t room = top_room(rows, vocab, k);
     if (room && (!workspace || !aligned(workspace, 16))) return SBC_EINVAL;
     if (workspace_bytes < room) return SBC_ECAPACITY;
+    const uint64_t listed = (uint64_t)rows * k * 4;
+    if (!apart({{index, listed}, {top, listed}, {lse, (uint64_t)rows * 4}, {workspace, room}}, {matrix_span(logits, type, rows, vocab, ld)})) return SBC_EINVAL;
     if (const int rc = device_status(device)) return rc;
     DeviceScope scope(device);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
@@ -346,14 +397,6 @@ bool distill_ok(const void* logits, int type, int64_t ld, int64_t rows, int64_t 
                 const float* weight) {
     return dim_ok(rows) && dense_ok(logits, type, vocab, ld) && index && top && aligned(index, 4) && aligned(top, 4) && aligned(teacher_lse, 4) && aligned(weight, 4) &&
            k >= 1 && k <= SBC_TOP_MAX;
-}
-
-// The gradient in the logits' own place, or nowhere near them.
-bool apart(const void* logits, int64_t ld, const void* grad, int64_t ld_grad, int64_t rows, int64_t vocab, size_t size) {
-    if (logits == grad) return ld == ld_grad;
-    const uintptr_t a = reinterpret_cast<uintptr_t>(logits), b = reinterpret_cast<uintptr_t>(grad);
-    const uintptr_t an = (uintptr_t)((rows - 1) * ld + vocab) * size, bn = (uintptr_t)((rows - 1) * ld_grad + vocab) * size;
-    return a + an <= b || b + bn <= a;
 }
 
 DistillArgs distill_args(const int32_t* index, const float* top, const float* teacher_lse, const float* weight, int k, double temperature) {
@@ -406,10 +449,14 @@ int sbc_distill_loss(int device, void* hip_stream, const void* logits, int type,
     if (k < 1 || k > SBC_TOP_MAX || !dim_ok(vocab) || !temperature_ok(temperature) || !size_of(type)) return SBC_EINVAL;
     if (rows == 0) return SBC_OK;
     if (!distill_ok(logits, type, ld, rows, vocab, index, top, k, teacher_lse, weight) || !loss || !aligned(loss, 4) || !aligned(stats, 16)) return SBC_EINVAL;
-    if (grad && (!dense_ok(grad, type, vocab, ld_grad) || !apart(logits, ld, grad, ld_grad, rows, vocab, size_of(type)))) return SBC_EINVAL;
+    if (grad && (!dense_ok(grad, type, vocab, ld_grad) || (grad == logits && ld_grad != ld))) return SBC_EINVAL;
     const size_t room = sbc_distill_workspace(rows, vocab);
     if (room && (!workspace || !aligned(workspace, 16))) return SBC_EINVAL;
     if (workspace_bytes < room) return SBC_ECAPACITY;
+    const uint64_t listed = (uint64_t)rows * k * 4, each = (uint64_t)rows * 4;
+    // (in place the logits are what is written)
+    if (!apart({{loss, each}, {stats, 4 * each}, {workspace, room}, matrix_span(grad, type, rows, vocab, ld_grad)},
+               {matrix_span(grad == logits ? nullptr : logits, type, rows, vocab, ld), {index, listed}, {top, listed}, {teacher_lse, each}, {weight, each}})) return SBC_EINVAL;
     if (const int rc = device_status(device)) return rc;
     DeviceScope scope(device);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
@@ -446,7 +493,10 @@ int sbc_distill_grad(int device, void* hip_stream, const void* logits, int type,
     if (k < 1 || k > SBC_TOP_MAX || !dim_ok(vocab) || !temperature_ok(temperature) || !size_of(type)) return SBC_EINVAL;
     if (rows == 0) return SBC_OK;
     if (!distill_ok(logits, type, ld, rows, vocab, index, top, k, teacher_lse, dloss) || !stats || !aligned(stats, 16)) return SBC_EINVAL;
-    if (!dense_ok(grad, type, vocab, ld_grad) || !apart(logits, ld, grad, ld_grad, rows, vocab, size_of(type))) return SBC_EINVAL;
+    if (!dense_ok(grad, type, vocab, ld_grad) || (grad == logits && ld_grad != ld)) return SBC_EINVAL;
+    const uint64_t listed = (uint64_t)rows * k * 4, each = (uint64_t)rows * 4;
+    if (!apart({matrix_span(grad, type, rows, vocab, ld_grad)},
+               {matrix_span(grad == logits ? nullptr : logits, type, rows, vocab, ld), {index, listed}, {top, listed}, {teacher_lse, each}, {stats, 4 * each}, {dloss, each}})) return SBC_EINVAL;
     if (const int rc = device_status(device)) return rc;
     DeviceScope scope(device);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
