@@ -445,6 +445,10 @@ def sbc_last_route(ctx) -> int:
 
 
 # ------------------------------------------------ operators without a context
+#
+# Autograd records none of these calls: what requires a gradient gets one only by the calls that compute it
+# (sbc_distill_grad or sbc_distill_loss's grad, handed to logits.backward(); the products of a layer's by_cols forms).  What
+# a call writes counts as written, though.
 
 class Mxfp:
     """A rows x cols matrix in 4 bits: its container (uint8 device tensor of sbc_mxfp_bytes(rows, cols) bytes, made
@@ -456,11 +460,11 @@ class Mxfp:
             raise ValueError("a container holds at least one row and one column")
         if tensor is None:
             tensor = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        _check_device(tensor)
-        if tensor.dtype != torch.uint8 or not tensor.is_contiguous() or tensor.numel() < nbytes:
-            raise ValueError("a container is a contiguous uint8 tensor of sbc_mxfp_bytes(rows, cols) bytes")
+        device = tensor.get_device()
+        if device < 0 or tensor.dtype != torch.uint8 or not tensor.is_contiguous() or tensor.numel() < nbytes:
+            raise ValueError("a container is a contiguous uint8 device tensor of sbc_mxfp_bytes(rows, cols) bytes")
         self.rows, self.cols, self.tensor = rows, cols, tensor
-        self.ptr, self.device = tensor.data_ptr(), tensor.get_device()
+        self.ptr, self.device = tensor.data_ptr(), device
 
 
 # (the sizes below follow from their arguments alone, and a call through ctypes takes a microsecond)
@@ -469,20 +473,21 @@ def sbc_mxfp_bytes(rows: int, cols: int) -> int:
     return load().sbc_mxfp_bytes(rows, cols)
 
 
-def _same_device(on: int, device: int, what: str) -> None:
-    if on != device:
-        raise ValueError("%s must lie on the device of the call's first matrix" % what)
+def _elsewhere(what: str) -> ValueError:
+    return ValueError("%s must lie on the device of the call's first matrix" % what)
 
 
 def _dense(t: torch.Tensor, what: str, device: Optional[int] = None):
     """(pointer, type, rows, columns, leading dimension) of a matrix whose columns lie side by side; on `device` if given."""
-    _check_device(t)
     if device is not None:
-        _same_device(t.get_device(), device, what)
-    kind = SBC_TYPES.get(t.dtype)
-    if kind is None or t.dim() != 2:
+        if t.get_device() != device:
+            raise _elsewhere(what)
+    elif not t.is_cuda:
+        raise ValueError("libsbc works on device memory: expected a CUDA/HIP tensor")
+    kind, shape = SBC_TYPES.get(t.dtype), t.shape
+    if kind is None or len(shape) != 2:
         raise ValueError("%s must be a matrix of float32, bfloat16 or float16" % what)
-    rows, cols = t.shape
+    rows, cols = shape
     ld, step = t.stride()
     if step != 1 and cols > 1:
         raise ValueError("%s must have its columns side by side" % what)
@@ -491,7 +496,8 @@ def _dense(t: torch.Tensor, what: str, device: Optional[int] = None):
 
 def _held(q: "Mxfp", device: int, what: str) -> int:
     """Pointer of a container."""
-    _same_device(q.device, device, what)
+    if q.device != device:
+        raise _elsewhere(what)
     return q.ptr
 
 
@@ -536,9 +542,16 @@ def _operator_stream(stream, device: torch.device):
     return stream.cuda_stream
 
 
-def _checked(rc: int, where: str) -> None:
+# (the function behind torch.autograd.graph.increment_version, without the sorting out of its argument: 0.13 us for 0.32)
+_count_written = getattr(torch._C, "_increment_version", torch.autograd.graph.increment_version)
+
+
+def _checked(rc: int, where: str, *written: Optional[torch.Tensor]) -> None:
+    """Raises unless the call was enqueued; what it writes then counts as written for autograd, which refuses to use a
+    tensor that it has saved and that has changed since."""
     if rc != SBC_OK:
         raise SbcError(rc, where)
+    _count_written([t for t in written if isinstance(t, torch.Tensor)])
 
 
 def sbc_mxfp_quantize(x: torch.Tensor, by_rows: Optional[Mxfp] = None, by_cols: Optional[Mxfp] = None, stream=None) -> None:
@@ -549,9 +562,12 @@ def sbc_mxfp_quantize(x: torch.Tensor, by_rows: Optional[Mxfp] = None, by_cols: 
         raise ValueError("by_rows must be a container of x's shape")
     if by_cols is not None and (by_cols.rows, by_cols.cols) != (cols, rows):
         raise ValueError("by_cols must be a container of the transposed shape")
-    _checked(load().sbc_mxfp_quantize(x.device.index, _operator_stream(stream, x.device), ptr, kind, rows, cols, ld,
-                                      _held(by_rows, x.device.index, "by_rows") if by_rows is not None else None,
-                                      _held(by_cols, x.device.index, "by_cols") if by_cols is not None else None), "sbc_mxfp_quantize")
+    on = x.device
+    device = on.index
+    _checked(load().sbc_mxfp_quantize(device, _operator_stream(stream, on), ptr, kind, rows, cols, ld,
+                                      _held(by_rows, device, "by_rows") if by_rows is not None else None,
+                                      _held(by_cols, device, "by_cols") if by_cols is not None else None), "sbc_mxfp_quantize",
+             by_rows.tensor if by_rows is not None else None, by_cols.tensor if by_cols is not None else None)
 
 
 def sbc_mxfp_dequantize(q: Mxfp, out: torch.Tensor, stream=None) -> None:
@@ -559,8 +575,9 @@ def sbc_mxfp_dequantize(q: Mxfp, out: torch.Tensor, stream=None) -> None:
     ptr, kind, rows, cols, ld = _dense(out, "out")
     if (q.rows, q.cols) != (rows, cols):
         raise ValueError("out must have the container's shape")
-    _checked(load().sbc_mxfp_dequantize(out.device.index, _operator_stream(stream, out.device), _held(q, out.device.index, "q"), rows, cols, ptr, kind, ld),
-             "sbc_mxfp_dequantize")
+    on = out.device
+    _checked(load().sbc_mxfp_dequantize(on.index, _operator_stream(stream, on), _held(q, on.index, "q"), rows, cols, ptr, kind, ld),
+             "sbc_mxfp_dequantize", out)
 
 
 def sbc_mxfp_matmul(a: Mxfp, b: Mxfp, out: torch.Tensor, stream=None) -> None:
@@ -568,9 +585,10 @@ def sbc_mxfp_matmul(a: Mxfp, b: Mxfp, out: torch.Tensor, stream=None) -> None:
     ptr, kind, m, n, ld = _dense(out, "out")
     if a.cols != b.cols or (a.rows, b.rows) != (m, n):
         raise ValueError("out must be a.rows x b.rows, and a and b have as many columns")
-    device = out.device.index
-    _checked(load().sbc_mxfp_matmul(device, _operator_stream(stream, out.device), _held(a, device, "a"), _held(b, device, "b"), m, n, a.cols, ptr, kind, ld),
-             "sbc_mxfp_matmul")
+    on = out.device
+    device = on.index
+    _checked(load().sbc_mxfp_matmul(device, _operator_stream(stream, on), _held(a, device, "a"), _held(b, device, "b"), m, n, a.cols, ptr, kind, ld),
+             "sbc_mxfp_matmul", out)
 
 
 @functools.lru_cache(maxsize=4096)
@@ -581,14 +599,16 @@ def sbc_mxfp_linear_workspace(m: int, k: int) -> int:
 def sbc_mxfp_linear(x: torch.Tensor, w: Mxfp, out: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """out[M, N] = Q(x) w^T for x[M, K], rounded to 4 bits within the call, and a container w of N x K; one token or many."""
     xp, kind, m, k, ldx = _dense(x, "x")
-    device = x.device.index
+    on = x.device
+    device = on.index
     yp, out_kind, rows, n, ldy = _dense(out, "out", device)
     if w.cols != k or w.rows != n or rows != m or kind != out_kind:
         raise ValueError("x must be M x w.cols and out M x w.rows of the same type")
     lib = load()
-    keep, wp, wn = _scratch(sbc_mxfp_linear_workspace(m, k), workspace, x.device, stream)
-    _checked(lib.sbc_mxfp_linear(device, _operator_stream(stream, x.device), xp, kind, ldx, m, _held(w, device, "w"), n, k, yp, ldy, wp, wn),
-             "sbc_mxfp_linear")
+    room = sbc_mxfp_linear_workspace(m, k)
+    keep, wp, wn = _scratch(room, workspace, on, stream) if room else (None, None, 0)
+    _checked(lib.sbc_mxfp_linear(device, _operator_stream(stream, on), xp, kind, ldx, m, _held(w, device, "w"), n, k, yp, ldy, wp, wn),
+             "sbc_mxfp_linear", out)
 
 
 @functools.lru_cache(maxsize=4096)
@@ -605,11 +625,12 @@ def sbc_top_logits(logits: torch.Tensor, index: torch.Tensor, top: torch.Tensor,
         raise ValueError("index must be rows x k")
     k = index.shape[1]
     lib = load()
-    keep, wp, wn = _scratch(sbc_top_logits_workspace(rows, vocab, k), workspace, logits.device, stream)
-    device = logits.device.index
-    _checked(lib.sbc_top_logits(device, _operator_stream(stream, logits.device), ptr, kind, ld, rows, vocab, k, temperature,
+    on = logits.device
+    keep, wp, wn = _scratch(sbc_top_logits_workspace(rows, vocab, k), workspace, on, stream)
+    device = on.index
+    _checked(lib.sbc_top_logits(device, _operator_stream(stream, on), ptr, kind, ld, rows, vocab, k, temperature,
                                 _vector(index, rows * k, torch.int32, device, "index"), _vector(top, rows * k, torch.float32, device, "top"),
-                                _vector(lse, rows, torch.float32, device, "lse"), wp, wn), "sbc_top_logits")
+                                _vector(lse, rows, torch.float32, device, "lse"), wp, wn), "sbc_top_logits", index, top, lse)
 
 
 @functools.lru_cache(maxsize=4096)
@@ -636,13 +657,14 @@ def sbc_distill_loss(logits: torch.Tensor, index: torch.Tensor, top: torch.Tenso
     k = index.shape[1]
     gp, ldg = _like(grad, logits, "grad") if grad is not None else (None, 0)
     lib = load()
-    keep, wp, wn = _scratch(sbc_distill_workspace(rows, vocab), workspace, logits.device, stream)
-    device = logits.device.index
-    _checked(lib.sbc_distill_loss(device, _operator_stream(stream, logits.device), ptr, kind, ld, rows, vocab,
+    on = logits.device
+    keep, wp, wn = _scratch(sbc_distill_workspace(rows, vocab), workspace, on, stream)
+    device = on.index
+    _checked(lib.sbc_distill_loss(device, _operator_stream(stream, on), ptr, kind, ld, rows, vocab,
                                   _vector(index, rows * k, torch.int32, device, "index"), _vector(top, rows * k, torch.float32, device, "top"), k,
                                   _vector(teacher_lse, rows, torch.float32, device, "teacher_lse"), temperature,
                                   _vector(weight, rows, torch.float32, device, "weight"), _vector(loss, rows, torch.float32, device, "loss"),
-                                  _vector(stats, rows * 4, torch.float32, device, "stats"), gp, ldg, wp, wn), "sbc_distill_loss")
+                                  _vector(stats, rows * 4, torch.float32, device, "stats"), gp, ldg, wp, wn), "sbc_distill_loss", loss, stats, grad)
 
 
 def sbc_distill_grad(logits: torch.Tensor, index: torch.Tensor, top: torch.Tensor, temperature: float, stats: torch.Tensor,
@@ -654,9 +676,10 @@ def sbc_distill_grad(logits: torch.Tensor, index: torch.Tensor, top: torch.Tenso
         raise ValueError("index must be rows x k")
     k = index.shape[1]
     gp, ldg = _like(grad, logits, "grad")
-    device = logits.device.index
-    _checked(load().sbc_distill_grad(device, _operator_stream(stream, logits.device), ptr, kind, ld, rows, vocab,
+    on = logits.device
+    device = on.index
+    _checked(load().sbc_distill_grad(device, _operator_stream(stream, on), ptr, kind, ld, rows, vocab,
                                      _vector(index, rows * k, torch.int32, device, "index"), _vector(top, rows * k, torch.float32, device, "top"), k,
                                      _vector(teacher_lse, rows, torch.float32, device, "teacher_lse"), temperature,
                                      _vector(stats, rows * 4, torch.float32, device, "stats"), _vector(dloss, rows, torch.float32, device, "dloss"), gp, ldg),
-             "sbc_distill_grad")
+             "sbc_distill_grad", grad)
