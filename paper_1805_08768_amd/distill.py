@@ -134,7 +134,7 @@ def distilled_rounds(teacher: Teacher, hidden: List[torch.Tensor], p: float, n_r
         if on_loss is not None:
             on_loss(rnd, client, learner.loss)
 
-    start = None if weight is None else [weight.reshape(-1).cpu().numpy()]
+    start = None if weight is None else [weight.detach().reshape(-1).float().cpu().numpy()]
     W, uploaded = rounds.run_rounds([vocab * width], p, len(hidden), n_rounds, local_update, weights=start, device=device, on_device=True)
     return W[0].view(vocab, width), uploaded, down
 
