@@ -119,14 +119,15 @@ def distilled_rounds(teacher: Teacher, hidden: List[torch.Tensor], p: float, n_r
     """n_rounds of Alg. 1 with one client for each of `hidden` (its positions' hidden states, [positions, hidden] each), which
     learn teacher's layer.  weight: the server's first weights [vocab, hidden] (default zeros); share: per client,
     the positions' weights in its loss (default 1 / positions).  on_loss(round, client, losses of the last local step).
-    Returns the final weights, the bytes uploaded per round, and the bytes that a client downloads per round."""
+    Returns the final weights, the bytes uploaded per round, and the bytes that the client with the most positions downloads
+    for a round with its answers."""
     vocab, width = teacher.vocab, teacher.hidden
     device = str(hidden[0].device)
     if share is None:
         share = [torch.full((h.shape[0],), 1.0 / h.shape[0], device=device) for h in hidden]
     answers = [teacher.answer(h) for h in hidden]
     learners = [Learner(vocab, width, h.shape[0], teacher.temperature, lr, steps, device) for h in hidden]
-    down = learners[0].layer.nbytes + answers[0].nbytes
+    down = max(learner.layer.nbytes + a.nbytes for learner, a in zip(learners, answers))
 
     def local_update(client, rnd, W, out):
         learner = learners[client]

@@ -79,3 +79,11 @@ def test_first_weights_of_any_type(make):
     got, up_too, _ = distill.distilled_rounds(teacher, hidden, P, 2, LR, weight=make(weight.to(torch.float16).float()))
     same, up_same, _ = distill.distilled_rounds(teacher, hidden, P, 2, LR, weight=weight.to(torch.float16).float())
     assert up_too == up_same and torch.equal(got, same) and torch.isfinite(want).all()
+
+
+def test_the_largest_clients_download():
+    teacher, hidden = clients()
+    one = VOCAB, WIDTH
+    for order in (hidden, hidden[::-1]):
+        _, _, down = distill.distilled_rounds(teacher, order, P, 1, LR)
+        assert down == sbc.sbc_mxfp_bytes(*one) + 90 * (16 * 8 + 4)
