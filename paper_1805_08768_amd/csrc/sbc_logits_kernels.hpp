@@ -786,8 +786,9 @@ __device__ __forceinline__ void list_sums(ListSums& l, const Slots& z, const Dis
 }
 
 // The row's loss (before its weight) and what its gradient needs, from the sum over what is not listed.  Even and odd lanes
-// have one function each of two numbers worked out at a time.
-__device__ __forceinline__ float distill_row(const ListSums& l, ExpSum rest, const DistillArgs& a, DistillStats& st) {
+// have one function each of two numbers worked out at a time.  (In 64 bits, for the weight may bring a loss that 32 do not hold,
+// of a word masked by the lowest value, back among the numbers that they do.)
+__device__ __forceinline__ double distill_row(const ListSums& l, ExpSum rest, const DistillArgs& a, DistillStats& st) {
     const bool odd = threadIdx.x & 1u;
     const float m = fmaxf(rest.base, l.peak), top = finite_base(m);
     const bool empty = rest.base == -__builtin_inff() && rest.sum == 0.0f;
@@ -819,7 +820,7 @@ __device__ __forceinline__ float distill_row(const ListSums& l, ExpSum rest, con
     st.share = (float)((on ? l.total + p_rest : l.total) * of_sum);
     const bool none = !l.any || (m == -__builtin_inff() && sum == 0.0);
     if (none) st = {0.0f, 0.0f, 0.0f, -1.0f};
-    return none ? 0.0f : (float)(loss * (double)a.t * (double)a.t);
+    return none ? 0.0 : loss * (double)a.t * (double)a.t;
 }
 
 // Gradient of the listed entries.
@@ -959,9 +960,9 @@ __global__ __launch_bounds__(threads + 64) void k_distill_row(const T* logits, i
         list_sums(l, z, a, row, room, same);
         __syncthreads();
         DistillStats st;
-        const float loss = distill_row(l, block_sum(sums, threads / 64, a.c), a, st);
+        const double loss = distill_row(l, block_sum(sums, threads / 64, a.c), a, st);
         if (threadIdx.x == threads) {
-            out.loss[row] = weight * loss;
+            out.loss[row] = (float)(weight * loss);
             if (out.stats) out.stats[row] = st;
             shared = st;
         }
@@ -1052,9 +1053,9 @@ __global__ __launch_bounds__(kRowThreads) void k_distill(const T* logits, int64_
     if (threadIdx.x < 64) {
         list_sums(l, z, a, row, room, same);
         DistillStats st;
-        const float loss = distill_row(l, rest, a, st);
+        const double loss = distill_row(l, rest, a, st);
         if (threadIdx.x == 0) {
-            out.loss[row] = weight * loss;
+            out.loss[row] = (float)(weight * loss);
             if (out.stats) out.stats[row] = st;
             shared = st;
         }
@@ -1125,9 +1126,9 @@ __global__ __launch_bounds__(64) void k_distill_join(const T* __restrict__ logit
     ListSums l;
     list_sums(l, z, a, row, room, true);
     DistillStats st;
-    const float loss = distill_row(l, wave_join(s, a.c), a, st);
+    const double loss = distill_row(l, wave_join(s, a.c), a, st);
     if (threadIdx.x == 0) {
-        out.loss[row] = weight * loss;
+        out.loss[row] = (float)(weight * loss);
         if (out.stats) out.stats[row] = st;
     }
 }
