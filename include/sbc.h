@@ -411,6 +411,7 @@ int sbc_top_logits(int device, void* hip_stream, const void* logits, int type, i
  *   weight  device, rows, or NULL for 1: loss and gradient of a row are multiplied by it
  *   loss    device, rows
  *   stats   device, 16-byte aligned, rows x 4, or NULL: what sbc_distill_grad needs
+ *   temperature  in [1e-6, 1e6]
  *   grad    device, rows x vocab, or NULL: the gradient of the sum of the losses with respect to logits, in the same
  *           reading; logits itself (with the same ld) or memory that does not overlap it
  *   workspace  device, 16-byte aligned, sbc_distill_workspace(rows, vocab) bytes (NULL where that is 0) */

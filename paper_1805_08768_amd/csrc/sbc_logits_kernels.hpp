@@ -933,7 +933,8 @@ __device__ __forceinline__ void leave_out(const DistillOut& out, int64_t row) {
 // list: it marks it before they need the marks, and its arithmetic (1 to 2 us of dependent steps in 64 bits) runs
 // beside their sum.  (Row and list are kept apart down to the weight's test: with both under way across it 5555 x 10602
 // took 84 registers instead of 80 and 69 us instead of 62.)  Memory bounds it where enough rows are under way: 700 x 10000 of
-// 32 bits with the gradient 13 us (56 MB, 4.3 TB/s), 5555 x 10602 of 16 bits 60 us (236 MB, 3.9 TB/s).
+// 32 bits with the gradient 13.4 us (54 MB, 4.1 TB/s), 5555 x 10602 of 16 bits 60 us (228 MB, 3.8 TB/s; one row in 16 has
+// weight 0 in these and the following figures, and is not read).
 template <typename T, int n, int threads>
 __global__ __launch_bounds__(threads + 64) void k_distill_row(const T* logits, int64_t ld, uint32_t vocab, DistillArgs a, DistillOut out, T* grad, int64_t ld_grad) {
     __shared__ __attribute__((aligned(16))) uint32_t marks[threads * n / 4];
@@ -1016,8 +1017,8 @@ __global__ __launch_bounds__(threads + 64) void k_distill_row(const T* logits, i
     __syncthreads();
 }
 
-// A longer row to a workgroup, read a second time for the gradient.  8192 x 131071 of 16 bits, the loss alone, 375 us (2.15 GB,
-// 5.7 TB/s); with the gradient 1000 x 50000 61 us (200 MB from memory, the second reading from nearer caches).
+// A longer row to a workgroup, read a second time for the gradient.  8192 x 131071 of 16 bits, the loss alone, 375 us (2.01 GB,
+// 5.4 TB/s); with the gradient 1000 x 50000 61 us (194 MB from memory, the second reading from nearer caches).
 template <typename T>
 __global__ __launch_bounds__(kRowThreads) void k_distill(const T* logits, int64_t ld, uint32_t vocab, DistillArgs a, DistillOut out, T* grad, int64_t ld_grad) {
     __shared__ uint32_t marks[kWindowVecs / 4];
@@ -1134,8 +1135,8 @@ __global__ __launch_bounds__(64) void k_distill_join(const T* __restrict__ logit
 }
 
 // ... and parts again for the gradient from what the loss left, in this call or a later one.  As in k_distill_row the list
-// has a wavefront of its own, which has the values ready when the others have stored theirs.  8192 x 131071 of 16 bits 795 us
-// (4.3 GB read and written, 5.4 TB/s: memory).
+// has a wavefront of its own, which has the values ready when the others have stored theirs.  8192 x 131071 of 16 bits 800 us
+// (4.16 GB read and written, 5.2 TB/s: memory).
 template <typename T>
 __global__ __launch_bounds__(kPartThreads + 64) void k_distill_grad(const T* logits, int64_t ld, uint32_t vocab, DistillArgs a, const DistillStats* __restrict__ stats,
                                                                    uint32_t parts, uint32_t part_vecs, T* grad, int64_t ld_grad) {

@@ -81,7 +81,7 @@ class Teacher:
 
 class Learner:
     """A client's local training: `steps` steps of gradient descent on the layer from the weights it downloaded,
-    against a teacher's answers.  Buffers are made once."""
+    against a teacher's answers; hidden states in float32.  Buffers are made once."""
 
     def __init__(self, vocab: int, hidden: int, positions: int, temperature: float, lr: float, steps: int = 1, device: str = "cuda:0"):
         self.temperature, self.lr, self.steps = float(temperature), float(lr), int(steps)
@@ -118,7 +118,8 @@ def distilled_rounds(teacher: Teacher, hidden: List[torch.Tensor], p: float, n_r
                      on_loss: Optional[Callable[[int, int, torch.Tensor], None]] = None) -> Tuple[torch.Tensor, List[int], int]:
     """n_rounds of Alg. 1 with one client for each of `hidden` (its positions' hidden states, [positions, hidden] each), which
     learn teacher's layer.  weight: the server's first weights [vocab, hidden] (default zeros); share: per client,
-    the positions' weights in its loss (default 1 / positions).  on_loss(round, client, losses of the last local step).
+    the positions' weights in its loss (default 1 / positions).  on_loss(round, client, losses of the last local step): called
+    on the client's stream with the learner's own buffer, which its next step overwrites.
     Returns the final weights, the bytes uploaded per round, and the bytes that the client with the most positions downloads
     for a round with its answers."""
     vocab, width = teacher.vocab, teacher.hidden
